@@ -28,7 +28,10 @@ namespace {
 
 constexpr int kTile = 64;       // tokens of K and V in LDS
 constexpr float kSlack = 6.0f;  // a reference may lag the maximum by this many powers of two
-constexpr float kFused = 1.0e9f;  // references below which the fused operation leaves an exact difference
+// References below which float32 holds the whole numbers next to them.  Beyond,
+// a reference is the nearest number that float32 has, up to half a step (32 at
+// 10^9) from the maximum: the weights leave float16's range.
+constexpr float kWhole = 16777216.0f;
 
 typedef __attribute__((address_space(3))) void lds_void;
 
@@ -217,7 +220,7 @@ __device__ __forceinline__ void step(const AttendArgs& a, Rows<T, D>& w, const T
     w.limit = over ? fmaxf(to + kSlack, mx) : w.limit;
     w.base = to;
     w.l *= f;
-    huge = huge || !(__builtin_fabsf(to) < kFused);
+    huge = huge || !(__builtin_fabsf(to) < kWhole);
     for (int d = 0; d < D / 32; ++d) w.o[d] *= f;
   }
   add<T, D>(w, *tile, a.scale2, lane, s);
@@ -355,7 +358,7 @@ __global__ __launch_bounds__(256, 2) void many_kernel(AttendArgs a) {
 
   const uint32_t off_k = k_offset<D>(wave, lane), off_v = v_offset<D>(wave, lane);
   uint32_t odd = 0;   // a value that is not finite at a place that some row may not see
-  bool huge = false;  // scores beyond kFused
+  bool huge = false;  // scores beyond kWhole
   load_tile<T, D>(a, tiles[0], tile_pages(page_s, p0, a.c.shift, c0, c1, lane), h, c0, c1, wave, off_k, off_v);
   int pg = tile_pages(page_s, p0, a.c.shift, c0 + kTile, c1, lane);  // of the next tile
   int at = 0;

@@ -1,0 +1,38 @@
+"""rt_paged_attention where scores are far from ordinary: so large that float32
+has no whole numbers for them left."""
+import pytest
+import torch
+
+from tests import serve_reference as S
+from tests.test_gpu_attention import _inputs, _run
+
+pytestmark = pytest.mark.gpu
+
+
+def _near_mean(got, cache, batch, q):
+    """Rows whose scores are all equal, in float32 too (the same operations on
+    the same numbers): weights are equal, so a row is the mean of the values it
+    sees.  Off by u = half a step in the rounded weight, 2^-24 for each addition
+    of the sums (as serve_reference counts them), u in the output."""
+    u, e, g = torch.finfo(q.dtype).eps / 2, 2.0 ** -24, q.shape[1] // cache["k"].shape[1]
+    qs = batch["q_start"].tolist()
+    for i, kl in enumerate(batch["kv_len"].tolist()):
+        vs, n = S.gather(cache, batch, i)[1], qs[i + 1] - qs[i]
+        for t in range(n):
+            mine = vs[:, :kl - n + t + 1].repeat_interleave(g, 0)
+            ref, mag = mine.mean(1), mine.abs().mean(1)
+            tol = (u + 2 * (kl / 4 + 72) * e) * mag * (1 + u) + u * ref.abs() + 2.0 ** -24
+            near = (got[qs[i] + t].double() - ref).abs() <= tol
+            assert bool(near.all()), (i, t, int((~near).sum()))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("rows,kv", [(3, 12), (40, 49), (150, 159), (40, 1500)])
+@pytest.mark.parametrize("value", [900, 1014, 1100, 2900, 4500, 5736, 5748, 7800, 8000, 30000])
+def test_scores_beyond_whole_numbers(dtype, rows, kv, value):
+    """q and k of 128 equal elements: scores of 2^23.6 to 2^33.8 powers of two
+    (2^24 at 1,014, 2^29 at 5,736, 10^9 at 7,828), all the same."""
+    cache, batch, q = _inputs([rows], [kv], 2, 1, 128, 64, dtype, 1)
+    cache["k"].fill_(value)
+    q.fill_(value)
+    _near_mean(_run(cache, batch, q), cache, batch, q)
