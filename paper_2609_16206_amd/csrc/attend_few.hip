@@ -188,7 +188,7 @@ __global__ __launch_bounds__(256, NT) void few_kernel(AttendArgs a) {
   }
   if (__syncthreads_or(bad || odd)) {
     for (int rr = wave; rr < n_rows; rr += 4)
-      row_by_place<T, D>(a, sq, s, h, run, rr, c0, c1);
+      row_by_place<T, D, true>(a, sq, s, h, run, rr, c0, c1);
     return;
   }
 
@@ -238,12 +238,13 @@ __global__ __launch_bounds__(256, NT) void few_kernel(AttendArgs a) {
       for (int w = 1; w < 4; ++w) x += o_s[(w * DT + j) * 64 + lane];
       out.put4(16 * j + 4 * lg, x, inv);
     }
-    if (wave == 0 && lg == 0) out.put_sum(m[nt] * a.scale2, lsum[nt]);
+    if (wave == 0 && lg == 0) out.put_sum(m[nt], lsum[nt]);
   }
 }
 
 // Join of the runs of the rows of tiles with more than one:
-//   out = sum_i f_i O_i / sum_i f_i l_i,  f_i = 2^(base_i - max base).
+//   out = sum_i f_i O_i / sum_i f_i l_i,  f_i = 2^((base_i - max base) unit),
+// in few_kernel's units (scores) as exact as the weights of one run.
 // Many runs, a row to a workgroup.  A wave's lanes are 16-byte pieces of 256 / D
 // runs; a row's runs are those that begin at or before its last place.
 template <class T, int D>
@@ -275,7 +276,7 @@ __global__ __launch_bounds__(256) void join_kernel(AttendArgs a) {
     for (int o = 32; o; o >>= 1) mx = fmaxf(mx, __shfl_xor(mx, o));
     mx = fmaxf(mx, base);
     const float to = mx == kLowest ? 0.0f : mx;
-    const float keep = __builtin_amdgcn_exp2f(base - to), f = __builtin_amdgcn_exp2f(ml.x - to);
+    const float keep = weight2(base, to, a.unit), f = weight2(ml.x, to, a.unit);
     base = mx;
     l = l * keep + f * ml.y;
     acc *= keep;
@@ -345,7 +346,7 @@ __global__ __launch_bounds__(256) void join_few_kernel(AttendArgs a) {
     float mx = fmaxf(ml.x, base);
     for (int o = 8; o; o >>= 1) mx = fmaxf(mx, __shfl_xor(mx, o));
     const float to = mx == kLowest ? 0.0f : mx;
-    const float keep = __builtin_amdgcn_exp2f(base - to), f = __builtin_amdgcn_exp2f(ml.x - to);
+    const float keep = weight2(base, to, a.unit), f = weight2(ml.x, to, a.unit);
     base = mx;
     l = l * keep + f * ml.y;
 #pragma unroll
@@ -447,7 +448,8 @@ AttendPlan plan_attend(int head_dim, const Batch& b, int hkv, int hq) {
   return p;
 }
 
-hipError_t launch_attend(int dtype, int head_dim, const AttendPlan& p, const AttendArgs& a, hipStream_t stream) {
+hipError_t launch_attend(int dtype, int head_dim, const AttendPlan& p, AttendArgs a, hipStream_t stream) {
+  a.unit = p.tile_rows > 32 ? kBaseUnit : a.scale2;
   if (dtype == 0)
     return head_dim == 64 ? launch<__bf16, 64>(0, p, a, stream) : launch<__bf16, 128>(0, p, a, stream);
   return head_dim == 64 ? launch<_Float16, 64>(1, p, a, stream) : launch<_Float16, 128>(1, p, a, stream);

@@ -358,7 +358,7 @@ __global__ __launch_bounds__(256, 2) void many_kernel(AttendArgs a) {
 
   const uint32_t off_k = k_offset<D>(wave, lane), off_v = v_offset<D>(wave, lane);
   uint32_t odd = 0;   // a value that is not finite at a place that some row may not see
-  bool huge = false;  // scores beyond kWhole
+  bool huge = false;  // scores beyond kWhole, or below float32 in powers of two
   load_tile<T, D>(a, tiles[0], tile_pages(page_s, p0, a.c.shift, c0, c1, lane), h, c0, c1, wave, off_k, off_v);
   int pg = tile_pages(page_s, p0, a.c.shift, c0 + kTile, c1, lane);  // of the next tile
   int at = 0;
@@ -378,13 +378,17 @@ __global__ __launch_bounds__(256, 2) void many_kernel(AttendArgs a) {
     step<T, D>(a, w, &tiles[at], &tiles[at ^ 1], now, h, t0, c1, wave, off_k, off_v, first, masked, lane, huge);
   }
 
+  const float l = w.l + __shfl_xor(w.l, 32);
+  // A row that sees places of the run, but no score above -inf: in powers of two
+  // (1.44 to a score's unit) finite scores may have ended there.
+  const bool some = w.see > c0 || (a.tree && (w.bits >> max(c0 - first, 0)) != 0);
+  huge = huge || (some && w.limit == kLowest && l == 0.0f);
   if (__syncthreads_or(bad || huge || odd)) {
     for (int rr = row0 + wave; rr < min(row0 + R, n_rows); rr += 4)
-      row_by_place<T, D>(a, sq, s, h, run, rr, c0, c1);
+      row_by_place<T, D, false>(a, sq, s, h, run, rr, c0, c1);
     return;
   }
   const int rr = wrow + col;
-  const float l = w.l + __shfl_xor(w.l, 32);
   if (rr >= n_rows) return;
   const RowOut<T, D> out(a, sq, h, run, rr);
   const float inv = l == 0.0f ? 0.0f : 1.0f / l;
@@ -394,7 +398,7 @@ __global__ __launch_bounds__(256, 2) void many_kernel(AttendArgs a) {
     for (int r = 0; r < 4; ++r)
       out.put4(32 * d + 8 * r + 4 * hf,
                f32x4{w.o[d][4 * r], w.o[d][4 * r + 1], w.o[d][4 * r + 2], w.o[d][4 * r + 3]}, inv);
-  if (hf == 0) out.put_sum(w.limit == kLowest ? kLowest : w.base, l);
+  if (hf == 0) out.put_sum(w.limit == kLowest ? kLowest : w.base / kBaseUnit, l);
 }
 
 template <class T, int D>

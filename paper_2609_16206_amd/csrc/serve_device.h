@@ -148,6 +148,10 @@ __device__ __forceinline__ RowTile row_tile(const AttendArgs& a, int64_t tile, i
   return {s, (int)row0, false};
 }
 
+// Powers of two to a unit of many_kernel's references (a power of two itself: whole
+// numbers stay exact), so large that a finite score's never overflows.
+constexpr float kBaseUnit = 0x1p64f;
+
 // A sequence, one of its row tiles and one of their runs.
 struct Run {
   int s, tile, split;  // s -1: none
@@ -232,7 +236,7 @@ struct RowOut {
       *(f32x4*)(a.part_o + part() * D + d0) = o;
     }
   }
-  // the base of the weights, a power of two, and their sum
+  // the base of the weights, in units, and their sum
   __device__ __forceinline__ void put_sum(float base, float l) const {
     if (split >= 0) a.part_ml[part()] = make_float2(base, l);
   }
@@ -241,10 +245,11 @@ struct RowOut {
 // One row, place by place, by one wave: for runs in which a place that some
 // row of the workgroup does not see holds a value that is not finite (weight 0
 // times it would not be 0 in a matrix product), a page lies outside the cache,
-// or scores are so large that many_kernel's exponent is not exact.  Lanes take 64
+// or scores are such that many_kernel's exponents do not serve.  Lanes take 64
 // places each for the scores and D / 64 elements each for the sum; only what the
-// row sees is used.
-template <class T, int D>
+// row sees is used.  kScores: references in scores, as few_kernel's, not in
+// kBaseUnit powers of two, as many_kernel's.
+template <class T, int D, bool kScores>
 __device__ void row_by_place(const AttendArgs& a, const Seq& sq, int s, int h, int split, int rr, int c0, int c1) {
   constexpr int E = D / 64;
   const int lane = (int)(threadIdx.x & 63), shift = a.c.shift, ps = 1 << shift;
@@ -296,7 +301,7 @@ __device__ void row_by_place(const AttendArgs& a, const Seq& sq, int s, int h, i
     else
       a.part_o[out.part() * D + E * lane + e] = o[e];
   }
-  if (lane == 0) out.put_sum(m * a.scale2, l);
+  if (lane == 0) out.put_sum(kScores ? m : m / kBaseUnit * a.scale2, l);
 }
 
 // Rows of a rejected sequence, as far as they lie in the tensors, from row

@@ -65,7 +65,8 @@ struct AttendArgs {
   int32_t hq, group, tile_rows, chunk, n_splits;
   float scale2;      // scale * log2(e)
   float* part_o;     // [n_splits][n_tokens * hq][head_dim]
-  float2* part_ml;   // [n_splits][n_tokens * hq] reference of the weights (a power of two) and their sum
+  float2* part_ml;   // [n_splits][n_tokens * hq] reference of the weights, in units, and their sum
+  float unit;        // powers of two to a unit: no finite score's reference leaves float32
 };
 
 struct SampleArgs {
@@ -84,7 +85,7 @@ struct SampleArgs {
 
 hipError_t launch_append(int dtype, int head_dim, const AppendArgs& a, hipStream_t stream);
 AttendPlan plan_attend(int head_dim, const Batch& b, int hkv, int hq);
-hipError_t launch_attend(int dtype, int head_dim, const AttendPlan& p, const AttendArgs& a, hipStream_t stream);
+hipError_t launch_attend(int dtype, int head_dim, const AttendPlan& p, AttendArgs a, hipStream_t stream);
 void launch_attend_many(int dtype, int head_dim, const AttendPlan& p, const AttendArgs& a, hipStream_t stream);
 int64_t sample_workspace(int64_t n_rows, int32_t vocab);
 hipError_t launch_sample(int dtype, const SampleArgs& a, hipStream_t stream);

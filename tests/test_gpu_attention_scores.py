@@ -1,5 +1,5 @@
 """rt_paged_attention where scores are far from ordinary: so large that float32
-has no whole numbers for them left."""
+has no whole numbers for them left, up to its largest and lowest ones."""
 import pytest
 import torch
 
@@ -36,3 +36,20 @@ def test_scores_beyond_whole_numbers(dtype, rows, kv, value):
     cache["k"].fill_(value)
     q.fill_(value)
     _near_mean(_run(cache, batch, q), cache, batch, q)
+
+
+@pytest.mark.parametrize("sign", [-1, 1])
+@pytest.mark.parametrize("rows,kv", [(1, 50), (1, 700), (1, 6000), (20, 700), (40, 49), (40, 3000), (150, 200)])
+def test_scores_at_the_ends_of_float32(rows, kv, sign):
+    """Scores of +-2.9e38, which float32 does not hold in powers of two (1.44
+    times as much), are scores like others, in one run and in several, by the
+    row's place and by a tree's words."""
+    cache, batch, q = _inputs([rows], [kv], 4, 2, 64, 64, torch.bfloat16, 1)
+    cache["k"].fill_(0)
+    cache["k"][..., 0] = sign * 1.7e19
+    q.fill_(0)
+    q[..., 0] = 1.7e19
+    _near_mean(_run(cache, batch, q, scale=1.0), cache, batch, q)
+    if rows <= 64:
+        tree = torch.tensor([(2 << t) - 1 for t in range(rows)], dtype=torch.int64)
+        _near_mean(_run(cache, batch, q, scale=1.0, tree=tree), cache, batch, q)
