@@ -177,7 +177,7 @@ __global__ __launch_bounds__(256, NT) void few_kernel(AttendArgs a) {
       float sum = 0.0f;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const float e = weight2(sc[nt][i >> 2][i & 3], base, a.scale2);
+        const float e = weight2(sc[nt][i >> 2][i & 3], base, a.scale2, raised<T>(0.0f));
         sum += e;
         p[i] = (T)e;
       }

@@ -49,9 +49,9 @@ __device__ __forceinline__ int swizzle(int t) {
 }
 
 // A wave's rows.  Weights are 2^(s scale2 - base), one fused operation and the
-// exponential, base a whole number per row close to the row's running maximum
-// of s scale2: it moves when a score is more than kSlack above it, and first
-// with the row's first seen score.  Weights and sums carry the same power of
+// exponential, base a whole number per row, raised<T> below or close to the row's
+// running maximum of s scale2: it moves when a score is more than kSlack above
+// that, and first with the row's first seen score.  Weights and sums carry the same power of
 // two, so a base below the maximum is no error, and a move is exact.
 template <class T, int D>
 struct Rows {
@@ -215,9 +215,9 @@ __device__ __forceinline__ void step(const AttendArgs& a, Rows<T, D>& w, const T
     // compiler copies O for every tile.)
     const bool over = mx > w.limit;
     if (!__ballot(over)) break;
-    const float to = over ? __builtin_rintf(mx) : w.base;
+    const float to = over ? __builtin_rintf(mx) - raised<T>(kSlack) : w.base;
     const float f = w.limit == kLowest ? 1.0f : __builtin_amdgcn_exp2f(w.base - to);
-    w.limit = over ? fmaxf(to + kSlack, mx) : w.limit;
+    w.limit = over ? fmaxf(to + (raised<T>(kSlack) + kSlack), mx) : w.limit;
     w.base = to;
     w.l *= f;
     huge = huge || !(__builtin_fabsf(to) < kWhole);

@@ -126,6 +126,21 @@ constexpr float kLowest = -__builtin_inff();
 __device__ __forceinline__ float weight2(float s, float base, float scale2) {
   return __builtin_amdgcn_exp2f((s - base) * scale2);
 }
+// The same times 2^up.
+__device__ __forceinline__ float weight2(float s, float base, float scale2, float up) {
+  return __builtin_amdgcn_exp2f(__builtin_fmaf(s - base, scale2, up));
+}
+
+// Powers of two by which weights are raised before they are rounded to T, so that
+// the largest stay below 2^16 (the largest of a row is 2^lag in many_kernel,
+// whose references lag): float16 holds 11 bits down to 2^-14 and nothing below
+// 2^-25, and a row's many small weights may be most of its sum.  Raised by 15, a
+// weight of 2^-29 of the largest keeps its bits (by 9, one of 2^-23), and none is off
+// by more than 2^-40 (2^-33) of it.  bfloat16 has float32's range.
+template <class T>
+constexpr float raised(float lag) {
+  return __is_same(T, __bf16) ? 0.0f : 15.0f - lag;
+}
 
 // The row tile of a workgroup (rows count in 32 bits, divided by the group's
 // size without the long way of 64): sequence s owns tiles
@@ -277,7 +292,7 @@ __device__ void row_by_place(const AttendArgs& a, const Seq& sq, int s, int h, i
     for (int i = 32; i; i >>= 1) mn = fmaxf(mn, __shfl_xor(mn, i));
     mn = fmaxf(mn, m);
     const float base = mn == kLowest ? 0.0f : mn;
-    const float f = weight2(m, base, a.scale2), w = weight2(x, base, a.scale2);
+    const float f = weight2(m, base, a.scale2), w = weight2(x, base, a.scale2, kScores ? raised<T>(0.0f) : 0.0f);
     m = mn;
     l = l * f + (vis ? w : 0.0f);
 #pragma unroll

@@ -1,5 +1,7 @@
 """rt_paged_attention where scores are far from ordinary: so large that float32
-has no whole numbers for them left, up to its largest and lowest ones."""
+has no whole numbers for them left, up to its largest and lowest ones, or far below others that count."""
+import math
+
 import pytest
 import torch
 
@@ -53,3 +55,31 @@ def test_scores_at_the_ends_of_float32(rows, kv, sign):
     if rows <= 64:
         tree = torch.tensor([(2 << t) - 1 for t in range(rows)], dtype=torch.int64)
         _near_mean(_run(cache, batch, q, scale=1.0, tree=tree), cache, batch, q)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("new,kv", [(1, 4000), (20, 4000), (40, 4000), (64, 1500)])
+@pytest.mark.parametrize("down", [14.5, 18.7, 22.45, 25.2, 28.3])
+def test_small_weights_add_up(dtype, new, kv, down):
+    """The first place outweighs every other 2^down times, but its values are
+    0: the others make the result.  Beside a thousand sequences without rows, so
+    that runs are long.  On top of serve_reference's bound a weight that float16
+    holds with fewer bits is off by at most 2^-33 of the largest."""
+    rows, kvs = [0] * 1100, [0] * 1100
+    rows[700], kvs[700] = new, kv
+    cache, batch, q = _inputs(rows, kvs, 1, 1, 64, 64, dtype, 1)
+    cache["k"].fill_(0)
+    cache["v"].abs_()
+    page = int(batch["page_table"][700, 0])
+    cache["k"][page, 0, 0, 0] = 8.0
+    cache["v"][page, 0, 0, :, 0] = 0.0
+    q.fill_(0)
+    q[..., 0] = 1.0
+    scale = down * math.log(2.0) / 8.0
+    got = _run(cache, batch, q, scale=scale)
+    ref, mag, big = S.attend(cache, batch, q, scale)
+    tol = S.attend_tolerance(ref, mag, big, dtype, kv, 64)
+    if dtype is torch.float16:
+        tol += kv * 2.0 ** -33 * float(cache["v"].max())
+    near = (got.double() - ref).abs() <= tol
+    assert bool(near.all()), (int((~near).sum()), float(((got.double() - ref).abs() / mag).max()))
