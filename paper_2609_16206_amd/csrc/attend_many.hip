@@ -156,9 +156,8 @@ __device__ __forceinline__ void add(Rows<T, D>& w, const Tile<T, D>& tile, float
   float sum = 0.0f;
 #pragma unroll
   for (int i = 0; i < 32; ++i) {
-    const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i >> 4][i & 15], scale2, -w.base));
-    sum += e;
-    p[i >> 3][i & 7] = (T)e;
+    p[i >> 3][i & 7] = (T)__builtin_amdgcn_exp2f(__builtin_fmaf(s[i >> 4][i & 15], scale2, -w.base));
+    if (i % 8 == 7) sum = sum8<T>(p[i >> 3], sum);
   }
   w.l += sum;
 #pragma unroll
@@ -171,11 +170,11 @@ __device__ __forceinline__ void add(Rows<T, D>& w, const Tile<T, D>& tile, float
   // V's first values are read and the first half's weights formed; then the
   // second half's weights beside the first half's products
   __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);
-  __builtin_amdgcn_sched_group_barrier(0x002, 56, 0);
+  __builtin_amdgcn_sched_group_barrier(0x002, 48, 0);
 #pragma unroll
   for (int i = 0; i < D / 16; ++i) {
     __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-    __builtin_amdgcn_sched_group_barrier(0x002, 896 / D, 0);
+    __builtin_amdgcn_sched_group_barrier(0x002, 768 / D, 0);
     if (D == 128) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
   }
   __builtin_amdgcn_sched_group_barrier(0x008, D / 16, 0);
