@@ -322,7 +322,7 @@ __device__ void row_by_place(const AttendArgs& a, const Seq& sq, int s, int h, i
     const uint64_t all = __ballot(vis);
     for (int i = 0; i < 64 && j0 + i < end; ++i) {
       if (!(all >> i & 1)) continue;
-      const float p = (float)(T)__shfl(w, i);
+      const float p = __shfl(w, i);  // (no matrix product: no rounding to T)
       const int pi = __shfl(pg, i), slot = (j0 + i) & (ps - 1);
       const T* v = (const T*)a.c.v + ((((int64_t)pi * a.c.hkv + h) << shift) + (slot & ~7)) * D + (slot & 7);
 #pragma unroll

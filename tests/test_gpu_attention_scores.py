@@ -96,3 +96,22 @@ def test_equal_values_are_their_mean(dtype, rows, kv):
     cache["v"].copy_(one.expand_as(cache["v"]))
     got = _run(cache, batch, q)
     assert torch.equal(got, one[0, :, 0, :, 0].repeat_interleave(3, 0).expand_as(got))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("rows", [3, 40])
+def test_rows_by_place_hold_their_weights_in_float32(dtype, rows):
+    """Next to values that some rows do not see and that are not finite, rows go
+    over their places one by one, with no matrix product and no rounding of
+    weights: serve_reference's bound without that part."""
+    cache, batch, q = _inputs([rows], [rows + 6], 4, 2, 64, 16, dtype, 3)
+    clean = {k: v.clone() for k, v in cache.items()}
+    place = rows + 5  # the last row's own
+    page = int(batch["page_table"][0, place // 16])
+    cache["v"][page, :, place % 16 // 8, :, place % 8] = math.inf
+    got = _run(cache, batch, q)[:-1]
+    ref, mag, big = (x[:-1] for x in S.attend(clean, batch, q, 0.125))
+    u = torch.finfo(dtype).eps / 2
+    tol = S.attend_tolerance(ref, mag, big, dtype, rows + 6, 64) - u * mag * (1 + u)
+    near = (got.double() - ref).abs() <= tol
+    assert bool(near.all()), int((~near).sum())
