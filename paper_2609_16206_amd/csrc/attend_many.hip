@@ -262,7 +262,7 @@ __device__ __forceinline__ RowTile costliest(const AttendArgs& a, int rank) {
   const int lane = (int)(threadIdx.x & 63), unit = R / a.group;
   int b = 0, t = 0;
   if (lane < a.b.n_seqs) {
-    const int rows = max(max(min(a.b.q_start[lane + 1], a.b.n_tokens), 0) - max(a.b.q_start[lane], 0), 0);
+    const int rows = rows_in(a.b, lane);
     const int kvl = a.b.kv_len[lane];
     t = (int)(((int64_t)rows * a.group + R - 1) / R);
     b = kvl >= rows && kvl <= a.b.max_kv ? (kvl - rows) / unit : 0;  // (else rejected)

@@ -164,23 +164,28 @@ constexpr float raised(float lag) {
   return __is_same(T, __bf16) ? 0.0f : 15.0f - lag;
 }
 
+// Where sequence i's rows start in the tensors, whatever q_start says.  Every
+// way from a workgroup to its tile counts rows by it, as reject_rows does.
+__device__ __forceinline__ int row_start(const Batch& b, int i) { return min(max(b.q_start[i], 0), b.n_tokens); }
+__device__ __forceinline__ int rows_in(const Batch& b, int i) { return max(row_start(b, i + 1) - row_start(b, i), 0); }
+
 // The row tile of a workgroup (rows count in 32 bits, divided by the group's
 // size without the long way of 64): sequence s owns tiles
-// floor(q_start[s] group / tile_rows) + s and up, or tile s alone where one
+// floor(row_start(s) group / tile_rows) + s and up, or tile s alone where one
 // holds any sequence's rows.
 struct RowTile {
   int s;         // -1: none
-  int row0;  // its first row within the sequence
+  int row0;      // its first row within the sequence
   bool one;
 };
 
 __device__ __forceinline__ RowTile row_tile(const AttendArgs& a, int64_t tile, int tile_rows) {
-  const int32_t* q = a.b.q_start;
+  const Batch& b = a.b;
   const int64_t G = a.group;
   if (a.b.max_q * G <= tile_rows) return {(int)tile, 0, true};
   const int s = __builtin_amdgcn_readfirstlane(
-      wave_count_le([q, G, tile_rows](int i) { return q[i] * G / tile_rows + i; }, a.b.n_seqs, tile) - 1);
-  const int64_t row0 = s < 0 ? 0 : (tile - (q[s] * G / tile_rows + s)) * tile_rows;
+      wave_count_le([&b, G, tile_rows](int i) { return row_start(b, i) * G / tile_rows + i; }, b.n_seqs, tile) - 1);
+  const int64_t row0 = s < 0 ? 0 : (tile - (row_start(b, s) * G / tile_rows + s)) * tile_rows;
   if (row0 < 0 || row0 > kMostRows) return {-1, 0, false};
   return {s, (int)row0, false};
 }
@@ -218,8 +223,7 @@ __device__ __forceinline__ Run nth_run(const AttendArgs& a, int rank, bool one) 
     return q0 == q1 || !accepted(a.b, q0, q1, kvl) ? 1 : (int)((uint32_t)(kvl + a.chunk - 1) / (uint32_t)a.chunk);
   };
   auto tiles = [&](int i) {
-    const int rows = max(max(min(a.b.q_start[i + 1], a.b.n_tokens), 0) - max(a.b.q_start[i], 0), 0);
-    return one ? 1 : max((int)((uint32_t)(rows * a.group + a.tile_rows - 1) / (uint32_t)a.tile_rows), 1);
+    return one ? 1 : max((int)((uint32_t)(rows_in(a.b, i) * a.group + a.tile_rows - 1) / (uint32_t)a.tile_rows), 1);
   };
   auto find = [&](int count) {  // the lane whose counts reach the rank, which becomes the one among its own
     const int upto = wave_scan(count);
@@ -345,8 +349,8 @@ __device__ void row_by_place(const AttendArgs& a, const Seq& sq, int s, int h, i
 // `row0` of the sequence to `stop`: NaN.
 template <class T, int D>
 __device__ __forceinline__ void reject_rows(const AttendArgs& a, const Seq& sq, int s, int h, int64_t row0, int64_t stop) {
-  const int q1 = min(a.b.q_start[s + 1], a.b.n_tokens), q0 = max(sq.q0, 0);
-  stop = min(stop, (int64_t)(q1 - q0) * a.group);
+  const int q0 = row_start(a.b, s);
+  stop = min(stop, (int64_t)rows_in(a.b, s) * a.group);
   for (int64_t i = row0 * D + threadIdx.x; i < stop * D; i += blockDim.x) {
     const int64_t rr = i / D;
     ((T*)a.o.data)[(q0 + rr / a.group) * a.o.ts + (h * a.group + rr % a.group) * a.o.hs + i % D] =
