@@ -377,12 +377,12 @@ typedef struct {
  * without reading the device.  A sequence is rejected if its rows decrease or
  * end behind n_tokens, n > max_q, kv_len < n or kv_len > max_kv. */
 typedef struct {
-  int64_t n_seqs, n_tokens;  /* >= 0, < 2^31; n_tokens rows in the row tensors */
+  int64_t n_seqs, n_tokens;  /* >= 0, < 2^31 - 1; n_tokens rows in the row tensors */
   const int32_t* q_start;    /* [n_seqs + 1], non-decreasing                   */
   const int32_t* kv_len;     /* [n_seqs]                                       */
   const int32_t* page_table; /* [n_seqs][table_stride]                         */
   int64_t table_stride;      /* >= ceil(max_kv / page_size)                    */
-  int32_t max_q, max_kv;     /* >= 0                                           */
+  int32_t max_q, max_kv;     /* >= 0, max_kv <= 2^28                           */
 } rt_kv_batch;
 
 /* Rows of heads: element d of head h of row t at data[t * token_stride +
@@ -414,7 +414,7 @@ typedef struct {
  * cache place.  k_out of a row is rounded once to the cache's dtype.
  * A row of a rejected sequence, or whose page lies outside [0, n_pages), is
  * not written to the cache and its q_out is NaN.  Two rows at one place of one
- * page in one call race. */
+ * page in one call race.  Limits: n_tokens < 2^26 - 3, n_q_heads <= 65,536. */
 rt_status rt_kv_append(const rt_kv_cache* cache, const rt_kv_batch* batch, const rt_rope* rope,
                        const int32_t* positions, int32_t n_q_heads, const rt_heads* q, const rt_heads* q_out,
                        const rt_heads* k, const rt_heads* v, void* hip_stream);
@@ -435,7 +435,10 @@ rt_status rt_kv_append(const rt_kv_cache* cache, const rt_kv_batch* batch, const
  * workspace: rt_paged_attention_workspace bytes, 16-byte aligned, not shared
  * by calls that may run at once; NULL if that is 0.
  * n_q_heads is a multiple of n_kv_heads, at most 64 times as many; scale is
- * finite and > 0; n_tokens * n_q_heads <= 2^31 - 4,097. */
+ * finite and > 0.  Limits: n_tokens * n_q_heads <= 2^31 - 4,097, and fewer than
+ * 2^24 workgroups: of a sequence and KV head where max_q * (n_q_heads /
+ * n_kv_heads) <= 128, else of 128 such rows of a KV head, one more for each
+ * sequence (a call of at most 32 rows in several runs counts sequences alone). */
 rt_status rt_paged_attention(const rt_kv_cache* cache, const rt_kv_batch* batch, int32_t n_q_heads, float scale,
                              const rt_heads* q, const uint64_t* tree_mask, const rt_heads* out, void* workspace,
                              int64_t workspace_bytes, void* hip_stream);

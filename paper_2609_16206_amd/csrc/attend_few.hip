@@ -384,8 +384,8 @@ template <class T, int D, int NT>
 void launch_few(const AttendPlan& p, const AttendArgs& a, hipStream_t stream) {
   const int pages = (min((int64_t)p.chunk, (int64_t)a.b.max_kv) >> a.c.shift) + 2;
   const size_t lds = 4 * 16 * NT * sizeof(float2) + 4 * (D / 16) * 64 * sizeof(f32x4) + pages * sizeof(int);
-  const dim3 grid = p.n_splits == 1 || p.runs_in_a_row(a.c.hkv, a.b.n_seqs) ? dim3((uint32_t)(p.tiles * a.c.hkv * p.n_splits))
-                                                                : dim3((uint32_t)p.tiles, a.c.hkv, p.n_splits);
+  const uint32_t x = (uint32_t)p.groups_x(a.c.hkv, a.b.n_seqs);
+  const dim3 grid = p.n_splits == 1 || p.runs_in_a_row(a.c.hkv, a.b.n_seqs) ? dim3(x) : dim3(x, a.c.hkv, p.n_splits);
   few_kernel<T, D, NT><<<grid, 256, lds, stream>>>(a);
 }
 

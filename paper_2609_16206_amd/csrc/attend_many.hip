@@ -404,7 +404,7 @@ template <class T, int D>
 void launch(const AttendPlan& p, const AttendArgs& a, hipStream_t stream) {
   const int pages = (min((int64_t)p.chunk, (int64_t)a.b.max_kv) >> a.c.shift) + 2;
   const bool row = p.runs_in_a_row(a.c.hkv, a.b.n_seqs);
-  const dim3 grid((uint32_t)p.tiles * a.c.hkv * (row ? p.n_splits : 1), row ? 1 : p.n_splits);
+  const dim3 grid((uint32_t)p.groups_x(a.c.hkv, a.b.n_seqs), row ? 1 : p.n_splits);
   many_kernel<T, D><<<grid, 256, pages * sizeof(int), stream>>>(a);
 }
 

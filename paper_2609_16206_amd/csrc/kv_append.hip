@@ -157,7 +157,7 @@ hipError_t launch(const AppendArgs& a, hipStream_t stream) {
   // heads 44 us, one a workgroup 49); few leave compute units idle that way (512
   // rows 6.1 us, one a workgroup 5.1; 2,000 rows 10.9 and 10.2, 4,000 rows 18.0 and 18.8).
   if (a.b.n_tokens >= 10 * kComputeUnits)
-    append_kernel<T, D, 4><<<(a.b.n_tokens + 3) / 4, 256, 0, stream>>>(a);
+    append_kernel<T, D, kAppendRows><<<(a.b.n_tokens + kAppendRows - 1) / kAppendRows, 256, 0, stream>>>(a);
   else
     append_kernel<T, D, 1><<<a.b.n_tokens, 256, 0, stream>>>(a);
   return hipGetLastError();

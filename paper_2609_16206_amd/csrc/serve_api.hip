@@ -124,8 +124,8 @@ rt_status check_q_heads(const char* fn, int32_t hq, int32_t hkv) {
 // The plan of a call whose sizes have been checked, or RT_ERANGE.
 rt_status plan(const char* fn, const rt_kv_cache& c, const rt_kv_batch& b, int32_t hq, rt::AttendPlan* p) {
   *p = rt::plan_attend(c.head_dim, batch_of(b), c.n_kv_heads, hq);
-  if (p->tiles * c.n_kv_heads > kMaxInt || p->out_rows > rt::kMostRows)
-    return bad(RT_ERANGE, fn, "too many rows");
+  if (p->groups_x(c.n_kv_heads, (int32_t)b.n_seqs) > rt::kMostGroups || p->out_rows > rt::kMostRows)
+    return bad(RT_ERANGE, fn, "too many sequences or rows");
   return RT_OK;
 }
 
@@ -139,6 +139,8 @@ rt_status rt_kv_append(const rt_kv_cache* cache, const rt_kv_batch* batch, const
   const char* fn = "rt_kv_append";
   rt_status st;
   if ((st = check_cache(fn, cache)) != RT_OK || (st = check_sizes(fn, cache, batch)) != RT_OK) return st;
+  if ((batch->n_tokens + rt::kAppendRows - 1) / rt::kAppendRows > rt::kMostGroups)
+    return bad(RT_ERANGE, fn, "n_tokens must be below 2^26 - 3");
   if (q && (n_q_heads < 1 || n_q_heads > 65536)) return bad(RT_EINVAL, "rt_kv_append", "n_q_heads must be in [1, 65536]");
   if (rope) {
     if (rope->rot_dim < 16 || rope->rot_dim > cache->head_dim || rope->rot_dim % 16 != 0)

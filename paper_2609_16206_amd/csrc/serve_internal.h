@@ -29,6 +29,8 @@ struct Heads {
   int64_t ts, hs;  // strides in elements
 };
 
+constexpr int kAppendRows = 4;  // of a workgroup of an append of many rows
+
 struct AppendArgs {
   Pages c;
   Batch b;
@@ -42,6 +44,10 @@ struct AppendArgs {
 // Rows of a call, over all heads, at most.
 constexpr int64_t kMostRows = INT32_MAX - 4096;
 
+// Workgroups of 256 threads in one dimension of a launch, at most: its work
+// items are counted in 32 bits.
+constexpr int64_t kMostGroups = (1 << 24) - 1;
+
 // A launch of attention: rows of one sequence and KV head are (token, query
 // head of the group) pairs, tile_rows of them to a workgroup; the cache is
 // cut into n_splits runs of `chunk` tokens that separate workgroups take.
@@ -54,6 +60,12 @@ struct AttendPlan {
   // Launched in one dimension, for nth_run, unless sequences or runs are very many.
   bool runs_in_a_row(int32_t hkv, int32_t n_seqs) const {
     return n_seqs <= 1024 && tiles * hkv * n_splits <= 1 << 20;
+  }
+  // Workgroups in x: few rows in runs go by sequence, KV head and run, many by
+  // tile and head, and run.
+  int64_t groups_x(int32_t hkv, int32_t n_seqs) const {
+    if (n_splits == 1 || runs_in_a_row(hkv, n_seqs)) return tiles * hkv * n_splits;
+    return tile_rows > 32 ? tiles * hkv : tiles;
   }
 };
 

@@ -223,3 +223,28 @@ def test_binding_refuses_rows_it_cannot_pass(rt):
             rt._heads(t, "q", torch.bfloat16, n, d, h)
     with pytest.raises(TypeError, match="GPU"):
         rt._same_gpu([("q", x)])
+
+
+def test_limits_of_a_launch(rt):
+    """Sizes that a launch cannot take come back before it, and the largest
+    sizes that it can are planned."""
+    n = C.c_int64()
+    plan = lambda hq=4, hkv=2, **kw: rt._lib.rt_paged_attention_workspace(  # noqa: E731
+        C.byref(_cache(rt, n_kv_heads=hkv)), C.byref(_batch(rt, **kw)), hq, C.byref(n))
+    assert plan(n_seqs=(1 << 23) - 1) == rt.RT_OK and plan(n_seqs=1 << 23) == rt.RT_ERANGE  # 2 KV heads: 2^24 pairs
+    assert "too many" in rt.rt_last_error()
+    assert _attend(rt, batch=_batch(rt, n_seqs=1 << 23)) == rt.RT_ERANGE
+    # tiles of 128 rows of prompts: n_tokens / 128 + n_seqs of each KV head
+    many = dict(max_q=200, max_kv=200, table_stride=20, n_seqs=1 << 22)
+    assert plan(hq=2, n_tokens=(1 << 29) - 128, **many) == rt.RT_OK
+    assert plan(hq=2, n_tokens=1 << 29, **many) == rt.RT_ERANGE
+    # few rows in several runs are launched by sequence, head and run
+    runs = dict(max_kv=40000, table_stride=3000)
+    assert plan(n_seqs=(1 << 24) - 1, **runs) == rt.RT_OK and plan(n_seqs=1 << 24, **runs) == rt.RT_ERANGE
+    assert plan(n_tokens=(1 << 29) - 1024) == rt.RT_ERANGE  # n_tokens * n_q_heads
+    assert plan(n_tokens=(1 << 29) - 1025) == rt.RT_OK
+    for tokens in ((1 << 26) - 3, (1 << 31) - 2):  # an append's rows by four
+        assert _append(rt, batch=_batch(rt, n_tokens=tokens)) == rt.RT_ERANGE
+        assert "n_tokens" in rt.rt_last_error()
+    assert _append(rt, hq=65537) == rt.RT_EINVAL
+    assert _append(rt, batch=_batch(rt, n_tokens=(1 << 31) - 1)) == rt.RT_ERANGE
