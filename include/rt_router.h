@@ -434,8 +434,8 @@ rt_status rt_kv_append(const rt_kv_cache* cache, const rt_kv_batch* batch, const
  * page lies outside [0, n_pages).
  * workspace: rt_paged_attention_workspace bytes, 16-byte aligned, not shared
  * by calls that may run at once; NULL if that is 0.
- * n_q_heads is a multiple of n_kv_heads, at most 64 times as many; scale is
- * finite and > 0.  Limits: n_tokens * n_q_heads <= 2^31 - 4,097, and fewer than
+ * n_q_heads is a multiple of n_kv_heads, at most 64 times as many; scale is > 0
+ * and <= 2^127.  Limits: n_tokens * n_q_heads <= 2^31 - 4,097, and fewer than
  * 2^24 workgroups: of a sequence and KV head where max_q * (n_q_heads /
  * n_kv_heads) <= 128, else of 128 such rows of a KV head, one more for each
  * sequence (a call of at most 32 rows in several runs counts sequences alone). */

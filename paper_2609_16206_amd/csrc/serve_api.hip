@@ -202,6 +202,7 @@ rt_status rt_paged_attention(const rt_kv_cache* cache, const rt_kv_batch* batch,
       (st = check_q_heads(fn, n_q_heads, cache->n_kv_heads)) != RT_OK)
     return st;
   if (!std::isfinite(scale) || scale <= 0.0f) return bad(RT_EINVAL, "rt_paged_attention", "scale must be finite and > 0");
+  if (scale > 0x1p127f) return bad(RT_ERANGE, "rt_paged_attention", "scale > 2^127");  // (times log2(e): still a float)
   if (tree_mask && batch->max_q > 64) return bad(RT_ERANGE, "rt_paged_attention", "a tree has at most 64 new tokens");
   if (batch->n_tokens == 0 || batch->n_seqs == 0) return RT_OK;
   if ((st = check_arrays(fn, cache, batch)) != RT_OK) return st;

@@ -248,3 +248,14 @@ def test_limits_of_a_launch(rt):
         assert "n_tokens" in rt.rt_last_error()
     assert _append(rt, hq=65537) == rt.RT_EINVAL
     assert _append(rt, batch=_batch(rt, n_tokens=(1 << 31) - 1)) == rt.RT_ERANGE
+
+
+def test_scales_that_overflow_are_refused(rt):
+    """Scores are held in powers of two, 1.44 to a score's unit: scale times that
+    has to be a float32."""
+    for scale in (2.0 ** 127 * 1.01, 3e38, 3.4e38):
+        assert _attend(rt, scale=scale) == rt.RT_ERANGE
+        assert "2^127" in rt.rt_last_error()
+    # (the largest scale passes this check: the next one refuses the rows)
+    assert _attend(rt, scale=2.0 ** 127, batch=_batch(rt, max_q=65), tree=PTR) == rt.RT_ERANGE
+    assert "tree" in rt.rt_last_error()
