@@ -81,13 +81,15 @@ class Instance:
             raise ValueError(f"max_kv must be at most {self.max_len}")
         i32 = dict(dtype=torch.int32, device=self.device)
         return dict(q_start=torch.tensor([0] + list(np.cumsum(new)), **i32), kv_len=torch.tensor(list(total), **i32),
-                    page_table=self.page_table[:len(new)], max_q=max(list(new) + [0]),
+                    page_table=self.page_table[:len(new)], n_tokens=sum(new), max_q=max(list(new) + [0]),
                     max_kv=max(list(total) + [0, max_kv]))
 
     def forward(self, tokens: torch.Tensor, batch: Dict) -> torch.Tensor:
-        """Appends the tokens of every request and returns the logits
-        [requests, vocab] behind each one's last token."""
+        """Appends the tokens (below vocab) of every request and returns the
+        logits [requests, vocab] behind each one's last token."""
         s, n, d = self.shape, tokens.numel(), self.shape.head_dim
+        if n != batch.get("n_tokens", n):
+            raise ValueError(f"the batch brings {batch['n_tokens']} tokens, got {n}")
         hq, hkv = s.q_heads, s.kv_heads
         rope = dict(inv_freq=self.inv_freq)
         x = self.embed[tokens]

@@ -64,3 +64,14 @@ def test_batches_and_refusals():
 def test_measured_goes_with_calibrate_only():
     with pytest.raises(SystemExit):
         E.main(["policies", "--measured"])
+
+
+def test_tokens_must_match_the_batch():
+    """Too few or too many tokens come back before anything runs on them: rows
+    beyond the tensors would end the process on the GPU."""
+    inst = I.Instance(I.Shape(1, 2, 1, 64, 16, 24, 50), max_seqs=3, max_len=100, page_size=32, device="cpu")
+    for n in (0, 7, 9):
+        with pytest.raises(ValueError, match="8 tokens"):
+            inst.forward(torch.zeros(n, dtype=torch.int32), inst.batch([1, 7], [128, 7]))
+    with pytest.raises(ValueError, match="2 tokens"):
+        I.Decoder(inst, torch.zeros(1, dtype=torch.int32), [3, 4], 5, graph=False).step()
