@@ -54,6 +54,7 @@ __device__ __forceinline__ uint32_t order_key(float x) {
   const uint32_t u = __float_as_uint(x + 0.0f);
   return u ^ ((u >> 31) ? 0xffffffffu : 0x80000000u);
 }
+constexpr uint32_t kNoKey = 0x007fffffu;  // order_key(-inf): no key of a masked token lies above
 __device__ __forceinline__ float key_logit(uint32_t k) {
   return __uint_as_float(k ^ ((k >> 31) ? 0x80000000u : 0xffffffffu));
 }
@@ -170,10 +171,12 @@ struct Row {
   }
 };
 
-// The kept tokens: keys above `key`, and of its equals those up to `last`.
+// The kept tokens: keys above `key`, and of its equals those up to `last`.  Masked
+// tokens (-inf) stand last in the order and weigh nothing: they are in no list and
+// no count, or a mask that leaves few tokens would fill both.
 struct Kept {
-  uint32_t key = 0;
-  int last = 0x7fffffff;
+  uint32_t key = kNoKey;
+  int last = -1;
   __device__ __forceinline__ bool has(uint32_t k, int i) const { return k > key || (k == key && i <= last); }
 };
 
@@ -601,7 +604,7 @@ __global__ __launch_bounds__(kSegThreads) void stats_kernel(SampleArgs a) {
   if (kOrder) {
     uint32_t g = best;
     for (int o = 1; o < w.lanes; o <<= 1) g = max(g, (uint32_t)__shfl_xor(g, o));
-    if (lane % w.lanes == 0) w.group[(r * w.segs + seg) * (kSegThreads / w.lanes) + tid / w.lanes] = g;
+    if (lane % w.lanes == 0) w.group[(r * w.segs + seg) * (kSegThreads / w.lanes) + tid / w.lanes] = g > kNoKey ? g : 0;
     // ranges start at 0
     const int per = (kBins + w.segs - 1) / w.segs;
     for (int i = seg * per + tid; i < min((seg + 1) * per, kBins); i += kSegThreads) w.hist[r * kBins + i] = 0;
@@ -683,6 +686,7 @@ __global__ __launch_bounds__(kSegThreads) void order_kernel(SampleArgs a) {
       __syncthreads();  // (the next round writes the other half)
       if (part[bit & 1][0] + part[bit & 1][1] + part[bit & 1][2] + part[bit & 1][3] >= q.kk) bound = to;
     }
+    bound = max(bound, kNoKey + 1);
     Token* list = w.list + (r * w.segs + seg) * w.cap;
     row.template each<kC / 64>(c0, c1, lane, 64, [&](int i, float l) {
       const uint32_t key = order_key(l);
@@ -707,7 +711,7 @@ __global__ __launch_bounds__(kSegThreads) void order_kernel(SampleArgs a) {
     });
   else
     row.template each<4>(c0, c1, lane, 64, [&](int, float l) {
-      atomicAdd((unsigned long long*)&hist[range_of(l, q.lmax, s, kBins)], 1ull);
+      if (l > -kInf) atomicAdd((unsigned long long*)&hist[range_of(l, q.lmax, s, kBins)], 1ull);
     });
   __syncthreads();
   // (whole numbers: the order of these additions changes nothing)
@@ -764,7 +768,7 @@ __global__ __launch_bounds__(kSegThreads) void weigh_kernel(SampleArgs a) {
       Token* list = w.list + (r * w.segs + seg) * w.cap;
       row.template each<4>(c0, c1, lane, 64, [&](int i, float l) {
         const int b = range_of(l, q.lmax, s, kBins);
-        if (b > bin) return;
+        if (b > bin || l == -kInf) return;
         if (b == bin) {
           const int at = atomicAdd(&count, 1);
           if (at < w.cap) list[at] = Token{order_key(l), i};
