@@ -194,8 +194,6 @@ struct Shared : std::conditional_t<kOrder, List, NoList> {
   int starts[kMaxSegs];
   double table[kTable];
   uint64_t part[kWaves];
-  uint32_t key[kWaves], low[kWaves];
-  int idx[kWaves];
   int n_list, found;
   uint32_t min_key, max_key;
   uint64_t above;
