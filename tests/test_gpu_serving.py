@@ -1,6 +1,8 @@
 """The serving operators together: prompts in chunks beside single tokens,
 append -> attention -> draw, against float64 at every step; the instance that
 the measured calibration runs them in, eager and replayed."""
+import time
+
 import numpy as np
 import pytest
 import torch
@@ -221,3 +223,17 @@ def test_measured_calibration_end_to_end():
                       beta_dec=E.fit_batch_slowdown(cur["batch"], cur["step_ns"]))
     rows = E.run_cells([E.Cell("measured", pt, W.chat(4.0))], replicas=2, requests=200)
     assert 0 <= rows[0]["mean"] <= 1
+
+
+def test_measured_prefill_is_the_gpus_time():
+    """Host time between launches, here 50 ms a call, is no part of a prefill's
+    latency (a decode step's has none either: both are replayed)."""
+    from paper_2609_16206_amd import instance as I
+
+    class SlowHost(I.Instance):
+        def forward(self, tokens, batch):
+            time.sleep(0.05)
+            return super().forward(tokens, batch)
+    inst = SlowHost(I.Shape(**SMALL), max_seqs=1, max_len=160)
+    cur = I.measure(inst, prompts=(16, 100), outputs=(2,), batches=(1,), context=100, repeats=3)
+    assert all(0 < t < 2e7 for k in ("prefill_ns", "decode_ns", "step_ns") for t in cur[k])
