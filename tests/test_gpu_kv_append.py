@@ -171,3 +171,26 @@ def test_empty_calls():
     batch, n_pages, rows = S.make_batch([0, 0], [0, 4], 16, 1)
     kc, _, _ = _run(cache, batch, x, x)
     assert torch.equal(kc, cache["k"])
+
+
+@pytest.mark.parametrize("start", [[9, 0, 9], [0, 18, 9], [18, 9, 0], [5, -7, 30], [2 ** 31 - 1, -2 ** 31, 18]])
+@pytest.mark.parametrize("pad", [0, 3000])
+def test_rows_out_of_order_write_only_dealt_places(start, pad):
+    """Starts that decrease or lie far outside: whose row is whose is not
+    defined, but a row of q_out is the rotated one, NaN or as it was, and of
+    the cache only places that the table deals to the two sequences change."""
+    batch, n_pages, rows = S.make_batch([9, 9], [30, 20], 16, 1, pad_rows=pad)
+    cache = S.make_cache(n_pages, 1, 64, 16, torch.bfloat16, 2)
+    x = torch.randn(rows, 1, 64, generator=torch.Generator().manual_seed(3)).bfloat16()
+    batch["q_start"] = torch.tensor(start, dtype=torch.int32)
+    batch["max_q"] = rows
+    out = torch.full((rows, 1, 64), 7.0, dtype=torch.bfloat16)
+    kc, vc, qo = _run(cache, batch, x, x, x, out)
+    for r in range(rows):
+        assert torch.equal(qo[r], x[r]) or (qo[r] == 7.0).all() or torch.isnan(qo[r]).all()
+    dealt = {(int(batch["page_table"][i, p // 16]), p % 16) for i, n in enumerate((30, 20)) for p in range(n)}
+    for pg in range(n_pages):
+        for sl in range(16):
+            if (pg, sl) not in dealt:
+                assert torch.equal(kc[pg, :, sl], cache["k"][pg, :, sl])
+                assert torch.equal(vc[pg, :, sl // 8, :, sl % 8], cache["v"][pg, :, sl // 8, :, sl % 8])
