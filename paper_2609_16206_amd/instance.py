@@ -50,7 +50,7 @@ class Instance:
 
     def __init__(self, shape: Shape = Shape(), max_seqs: int = 64, max_len: int = 8192, dtype=torch.bfloat16,
                  page_size: int = 64, seed: int = 0, device="cuda"):
-        self.shape, self.dtype, self.device, self.max_seqs = shape, dtype, torch.device(device), max_seqs
+        self.shape, self.dtype, self.max_seqs = shape, dtype, max_seqs
         s, g = shape, torch.Generator(device).manual_seed(seed)
 
         def weight(n_out, n_in):
@@ -59,6 +59,7 @@ class Instance:
 
         d = s.head_dim
         self.embed = torch.randn(s.vocab, s.hidden, generator=g, device=device).to(dtype)
+        self.device = self.embed.device  # (with its number: the current GPU may be another one later)
         self.head = weight(s.vocab, s.hidden)
         self.layers = [dict(qkv=weight((s.q_heads + 2 * s.kv_heads) * d, s.hidden),
                             out=weight(s.hidden, s.q_heads * d), up=weight(2 * s.ffn, s.hidden),

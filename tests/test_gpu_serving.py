@@ -237,3 +237,12 @@ def test_measured_prefill_is_the_gpus_time():
     inst = SlowHost(I.Shape(**SMALL), max_seqs=1, max_len=160)
     cur = I.measure(inst, prompts=(16, 100), outputs=(2,), batches=(1,), context=100, repeats=3)
     assert all(0 < t < 2e7 for k in ("prefill_ns", "decode_ns", "step_ns") for t in cur[k])
+
+
+def test_an_instance_keeps_its_gpu():
+    """Made on "cuda", it names that GPU: what its calls allocate later lies
+    there, whichever is current then."""
+    from paper_2609_16206_amd import instance as I
+    inst = I.Instance(I.Shape(**SMALL), max_seqs=1, max_len=64)
+    assert inst.device == torch.device("cuda", torch.cuda.current_device())
+    assert inst.batch([1], [1])["kv_len"].device == inst.device
