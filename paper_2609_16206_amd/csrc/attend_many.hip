@@ -15,11 +15,11 @@
 // 32 products (1,024 cycles) with heads of 128 and about as many cycles of
 // exponentials, maxima, sums and conversions, which two waves a SIMD overlap in
 // part (3,800 cycles for both); heads of 64 halve the products alone.  Two prompts
-// of 8,192 tokens, 16 heads of 128: 585 us, 940 TFLOP/s (a large matrix product
-// reaches 1,407); four of 4,096, heads of 64: 184 us, 748 TFLOP/s.  Short prompts
-// pay about 6 us a workgroup for its start and end: 29 of 16 to 3,342 tokens 165
-// us, 643 TFLOP/s.  Raising the waves' priority around the products gains nothing
-// (585 to 594 us).
+// of 8,192 tokens, 16 heads of 128: 585 to 607 us, 905 to 940 TFLOP/s (a large
+// matrix product reaches 1,407); four of 4,096, heads of 64: 182 us, 755 TFLOP/s.
+// Short prompts pay about 6 us a workgroup for its start and end: 29 of 16 to 3,342
+// tokens 152 us, 696 TFLOP/s (159 to 167 us replayed in a graph).  Raising the
+// waves' priority around the products gains nothing (585 to 594 us).
 #include "lane_ops.h"
 #include "serve_device.h"
 
@@ -167,7 +167,8 @@ __device__ __forceinline__ void add(Rows<T, D>& w, const Tile<T, D>& tile, float
       const x8 vf = *(const x8*)(tile.v + ((2 * g + h) * D + 32 * d + col) * 8);
       w.o[d] = Half<T>::mma32(vf, p[g], w.o[d]);
     }
-  // V's first values are read and the first half's weights formed; then the
+  // V's first values are read and the first half's weights formed (48 operations a
+  // half: exponent, exponential, half a conversion and half a sum each); then the
   // second half's weights beside the first half's products
   __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);
   __builtin_amdgcn_sched_group_barrier(0x002, 48, 0);
@@ -256,7 +257,8 @@ __device__ __forceinline__ int wave_sum(int x) {
 // sequences, one a lane.  Tile t of sequence i costs b_i + t, b_i the places before
 // its new ones in units of the new tokens of a tile; `above(e)` tiles cost e or
 // more.  Ties go by sequence.  Longest first keeps the end of a launch short:
-// 29 prompts of 16 to 3,342 tokens 168 us, in the order of the rows 185.
+// 29 prompts of 16 to 3,342 tokens 167 us, in the order of the rows 187; 8 of up to
+// 4,096 tokens 158, in the order of the rows 160, last rows first 174.
 __device__ __forceinline__ RowTile costliest(const AttendArgs& a, int rank) {
   constexpr int R = 128;
   const int lane = (int)(threadIdx.x & 63), unit = R / a.group;

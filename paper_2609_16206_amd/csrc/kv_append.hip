@@ -4,8 +4,9 @@
 //   (a, b) -> scale (a cos - b sin, b cos + a sin),  angle = position * inv_freq[j]
 //
 // The angle is taken in turns and float64, reduced to half a turn exactly, and
-// only then rounded to float32 (error 2^-26 turns at any position); the
-// products are float32, and a value is rounded once, to the cache's type.
+// only then rounded to float32 (error 2^-26 turns, beside float64's own of
+// 2^-51 of the angle at far positions); the products are float32, and a value
+// is rounded once, to the cache's type.
 //
 // A workgroup takes kRows rows.  One wave per row finds its sequence and
 // place and the row's sines, once for all heads; then threads take 16 elements

@@ -23,13 +23,16 @@
 // Bound by its passes over the row, the first at HBM's rate and the others from
 // the last-level cache, by the weights' float64 operations (about 20 a logit), and for
 // few rows by the chain of small kernels.  512 x 100,003 float32 logits by temperature
-// alone 106 us (41 + 53 + 10 for kernels 1, 3, 4; one read at 4.9 TB/s is 42); 96 x
-// 151,936 bfloat16 of every kind of setting 74 us; one row of 32,000 with top-k, top-p
+// alone 104 us (40 + 53 + 10 for kernels 1, 3, 4; one read at 4.9 TB/s is 42); 96 x
+// 151,936 bfloat16 of every kind of setting 73 us; one row of 32,000 with top-k, top-p
 // and min-p 28 us.
 //
-// What no list holds (top_k beyond kFewTokens together with top-p, thousands of
-// equal logits at the border) is left to whole_row, one workgroup that goes over
-// the row again for every step.
+// What no list holds is left to whole_row, one workgroup that goes over the row
+// again for every step: top_k beyond kFewTokens together with top-p (one row of
+// 151,936 bfloat16 176 us, 96 rows 205 us, where top_k 50 takes 37 and 60),
+// thousands of equal logits at the border (342 and 414 us), and more tokens than a
+// list holds in fewer groups than top_k (a mask that leaves a block of 5,000, top_k
+// 200: 96 and 141 us).
 #include <algorithm>
 #include <type_traits>
 

@@ -141,9 +141,10 @@ __device__ __forceinline__ float weight2(float s, float base, float scale2, floa
 // Matrix products take 16-bit operands, so weights are rounded to T for O =
 // V^T P^T; float32 weights would go through products in float32, at a
 // sixteenth of the rate.  Their sum is taken of the rounded ones: an output is
-// then a mean of the values it sees, exactly theirs where they are equal, and
-// the rounding moves it by half a step of the weights' spread only (sum of the
-// unrounded: 40 % more error for prompts in float64's eyes, 2.3e-3 for 1.65e-3).
+// then a mean of the values it sees, exactly theirs where they are equal.  Against
+// float64, relative, 29 prompts in bfloat16 are off by 2.04e-3 (the sum of the
+// unrounded weights: 2.33e-3; output rounding alone: 1.64e-3), single tokens by
+// 1.75e-3 (1.75e-3; 1.66e-3), chunks in float16 by 2.86e-4 (2.93e-4; 2.07e-4).
 template <class T>
 __device__ __forceinline__ float sum8(typename Half<T>::x8 p, float c) {
   const typename Half<T>::x2 one = {(T)1.0f, (T)1.0f};
@@ -157,7 +158,7 @@ __device__ __forceinline__ float sum8(typename Half<T>::x8 p, float c) {
 // the largest stay below 2^16 (the largest of a row is 2^lag in many_kernel,
 // whose references lag): float16 holds 11 bits down to 2^-14 and nothing below
 // 2^-25, and a row's many small weights may be most of its sum.  Raised by 15, a
-// weight of 2^-29 of the largest keeps its bits (by 9, one of 2^-23), and none is off
+// weight of 2^-29 of the largest keeps its bits (by 9, one of 2^-22), and none is off
 // by more than 2^-40 (2^-33) of it.  bfloat16 has float32's range.
 template <class T>
 constexpr float raised(float lag) {

@@ -38,8 +38,9 @@ class Shape:
 
 def rope_frequencies(rot_dim: int, base: float = 1e6, factor: float = 1.0, device="cuda") -> torch.Tensor:
     """Angles per position of the rotated pairs, float64 [rot_dim / 2]:
-    base ** (-2 j / rot_dim), divided by `factor` for positions beyond the
-    trained ones."""
+    base ** (-2 j / rot_dim) / factor.  A factor above 1 slows every pair at every
+    position alike, so that positions up to that many times the trained ones turn
+    no further than those."""
     j = torch.arange(rot_dim // 2, dtype=torch.float64)
     return (base ** (-2.0 * j / rot_dim) / factor).to(device)
 
@@ -187,7 +188,7 @@ def measure(inst: Instance, prompts: Sequence[int] = (16, 64, 256, 512, 1024, 20
     token, the time of a lone request's o - 1 decode steps, and the time of a
     decode step with b requests of `context` tokens each.  All of it is replayed
     from graphs: the GPU's time, without the host's between launches (16 tokens
-    of the default shape 5.0 ms, launched one by one 6.3)."""
+    of the default shape 5.0 ms, launched one by one 5.7 to 6.3)."""
     dev = inst.device
     g = torch.Generator(dev).manual_seed(seed)
     vocab = inst.shape.vocab
