@@ -376,7 +376,7 @@ typedef struct {
  * max_q and max_kv bound n and kv_len; the launch is planned from them
  * without reading the device (a long cache is cut into runs by max_kv: far above
  * every kv_len it leaves fewer, longer ones: 64 requests of 2,000 tokens 30 us
- * with a bound of 10,241, 49 with 131,072).  A sequence is rejected if its rows decrease or
+ * with a bound of 10,241, 48 with 131,072).  A sequence is rejected if its rows decrease or
  * end behind n_tokens, n > max_q, kv_len < n or kv_len > max_kv. */
 typedef struct {
   int64_t n_seqs, n_tokens;  /* >= 0, < 2^31 - 1; n_tokens rows in the row tensors */

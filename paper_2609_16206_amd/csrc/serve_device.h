@@ -145,6 +145,7 @@ __device__ __forceinline__ float weight2(float s, float base, float scale2, floa
 // float64, relative, 29 prompts in bfloat16 are off by 2.04e-3 (the sum of the
 // unrounded weights: 2.33e-3; output rounding alone: 1.64e-3), single tokens by
 // 1.75e-3 (1.75e-3; 1.66e-3), chunks in float16 by 2.86e-4 (2.93e-4; 2.07e-4).
+// It costs 1 % of the chunks' time (490 -> 494 us), nothing elsewhere.
 template <class T>
 __device__ __forceinline__ float sum8(typename Half<T>::x8 p, float c) {
   const typename Half<T>::x2 one = {(T)1.0f, (T)1.0f};
