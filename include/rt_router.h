@@ -429,9 +429,8 @@ rt_status rt_kv_append(const rt_kv_cache* cache, const rt_kv_batch* batch, const
  * the j-th where bit j of its word is set (max_q <= 64 then).  A row that
  * sees nothing, or only scores of -inf, is 0.  What a row does not see never
  * reaches it, NaN and infinities included.  Scores, the softmax and sums are
- * float32; weights are rounded to the cache's dtype for the second product, and
- * summed as rounded, so a row is a mean of the values it sees; out is rounded
- * once and may not overlap the inputs.
+ * float32; weights are rounded to the cache's dtype for the second product;
+ * out is rounded once and may not overlap the inputs.
  * Rows of a rejected sequence are NaN, as is a row that sees a place whose
  * page lies outside [0, n_pages).
  * workspace: rt_paged_attention_workspace bytes, 16-byte aligned, not shared

@@ -174,9 +174,14 @@ __global__ __launch_bounds__(256, NT) void few_kernel(AttendArgs a) {
         m[nt] = mn;
       }
       x8 p;
+      float sum = 0.0f;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) p[i] = (T)weight2(sc[nt][i >> 2][i & 3], base, a.scale2, raised<T>(0.0f));
-      l[nt] += sum8<T>(p, 0.0f);
+      for (int i = 0; i < 8; ++i) {
+        const float e = weight2(sc[nt][i >> 2][i & 3], base, a.scale2, raised<T>(0.0f));
+        sum += e;
+        p[i] = (T)e;
+      }
+      l[nt] += sum;
 #pragma unroll
       for (int j = 0; j < DT; ++j) o[nt][j] = Half<T>::mma16(vf[j], p, o[nt][j]);
     }

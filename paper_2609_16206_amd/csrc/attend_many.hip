@@ -156,8 +156,9 @@ __device__ __forceinline__ void add(Rows<T, D>& w, const Tile<T, D>& tile, float
   float sum = 0.0f;
 #pragma unroll
   for (int i = 0; i < 32; ++i) {
-    p[i >> 3][i & 7] = (T)__builtin_amdgcn_exp2f(__builtin_fmaf(s[i >> 4][i & 15], scale2, -w.base));
-    if (i % 8 == 7) sum = sum8<T>(p[i >> 3], sum);
+    const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i >> 4][i & 15], scale2, -w.base));
+    sum += e;
+    p[i >> 3][i & 7] = (T)e;
   }
   w.l += sum;
 #pragma unroll
@@ -167,15 +168,15 @@ __device__ __forceinline__ void add(Rows<T, D>& w, const Tile<T, D>& tile, float
       const x8 vf = *(const x8*)(tile.v + ((2 * g + h) * D + 32 * d + col) * 8);
       w.o[d] = Half<T>::mma32(vf, p[g], w.o[d]);
     }
-  // V's first values are read and the first half's weights formed (48 operations a
-  // half: exponent, exponential, half a conversion and half a sum each); then the
+  // V's first values are read and the first half's weights formed (56 operations a
+  // half: exponent, exponential, addition and half a conversion each); then the
   // second half's weights beside the first half's products
   __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);
-  __builtin_amdgcn_sched_group_barrier(0x002, 48, 0);
+  __builtin_amdgcn_sched_group_barrier(0x002, 56, 0);
 #pragma unroll
   for (int i = 0; i < D / 16; ++i) {
     __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-    __builtin_amdgcn_sched_group_barrier(0x002, 768 / D, 0);
+    __builtin_amdgcn_sched_group_barrier(0x002, 896 / D, 0);
     if (D == 128) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
   }
   __builtin_amdgcn_sched_group_barrier(0x008, D / 16, 0);

@@ -20,8 +20,6 @@ template <>
 struct Half<__bf16> {
   typedef __bf16 x8 __attribute__((ext_vector_type(8)));
   typedef __bf16 x4 __attribute__((ext_vector_type(4)));
-  typedef __bf16 x2 __attribute__((ext_vector_type(2)));
-  static __device__ __forceinline__ float dot2(x2 a, x2 b, float c) { return __builtin_amdgcn_fdot2_f32_bf16(a, b, c, false); }
   static __device__ __forceinline__ f32x4 mma16(x8 a, x8 b, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
   }
@@ -33,8 +31,6 @@ template <>
 struct Half<_Float16> {
   typedef _Float16 x8 __attribute__((ext_vector_type(8)));
   typedef _Float16 x4 __attribute__((ext_vector_type(4)));
-  typedef _Float16 x2 __attribute__((ext_vector_type(2)));
-  static __device__ __forceinline__ float dot2(x2 a, x2 b, float c) { return __builtin_amdgcn_fdot2(a, b, c, false); }
   static __device__ __forceinline__ f32x4 mma16(x8 a, x8 b, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
   }
@@ -135,26 +131,14 @@ __device__ __forceinline__ float weight2(float s, float base, float scale2, floa
   return __builtin_amdgcn_exp2f(__builtin_fmaf(s - base, scale2, up));
 }
 
-// The sum of eight rounded weights and c, float32 (a dot product with ones takes
-// two, at most 2.5 * 2^-24 off, and reads subnormal numbers).
+// Weights are rounded to T for O = V^T P^T, because matrix products take 16-bit
+// operands; float32 ones would go through products at a sixteenth of the rate.
+// Their sum is taken of the unrounded weights: the output is off by half a step of
+// the mean of |v| at most, and by none where the largest weight (exactly 1, or
+// a power of two) outweighs the others.  (The sum of the rounded ones gives equal
+// values as they are, but is off by up to twice that where values differ: numerator
+// and denominator may be rounded apart.)
 //
-// Matrix products take 16-bit operands, so weights are rounded to T for O =
-// V^T P^T; float32 weights would go through products in float32, at a
-// sixteenth of the rate.  Their sum is taken of the rounded ones: an output is
-// then a mean of the values it sees, exactly theirs where they are equal.  Against
-// float64, relative, 29 prompts in bfloat16 are off by 2.04e-3 (the sum of the
-// unrounded weights: 2.33e-3; output rounding alone: 1.64e-3), single tokens by
-// 1.75e-3 (1.75e-3; 1.66e-3), chunks in float16 by 2.86e-4 (2.93e-4; 2.07e-4).
-// It costs 1 % of the chunks' time (490 -> 494 us), nothing elsewhere.
-template <class T>
-__device__ __forceinline__ float sum8(typename Half<T>::x8 p, float c) {
-  const typename Half<T>::x2 one = {(T)1.0f, (T)1.0f};
-  c = Half<T>::dot2(__builtin_shufflevector(p, p, 0, 1), one, c);
-  c = Half<T>::dot2(__builtin_shufflevector(p, p, 2, 3), one, c);
-  c = Half<T>::dot2(__builtin_shufflevector(p, p, 4, 5), one, c);
-  return Half<T>::dot2(__builtin_shufflevector(p, p, 6, 7), one, c);
-}
-
 // Powers of two by which weights are raised before they are rounded to T, so that
 // the largest stay below 2^16 (the largest of a row is 2^lag in many_kernel,
 // whose references lag): float16 holds 11 bits down to 2^-14 and nothing below

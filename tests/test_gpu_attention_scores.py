@@ -86,19 +86,6 @@ def test_small_weights_add_up(dtype, new, kv, down):
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
-@pytest.mark.parametrize("rows,kv", [(1, 1), (1, 3), (1, 900), (16, 40), (40, 40), (150, 150), (40, 2000)])
-def test_equal_values_are_their_mean(dtype, rows, kv):
-    """Places with the same values give rows those values bit for bit (a prompt's
-    first row sees one place alone): numerator and denominator hold the same
-    rounded weights, and float32's part of the error is far from half a step."""
-    cache, batch, q = _inputs([rows], [kv], 6, 2, 128, 64, dtype, 3, 2.0)
-    one = cache["v"][:1, :, :1, :, :1].clone()
-    cache["v"].copy_(one.expand_as(cache["v"]))
-    got = _run(cache, batch, q)
-    assert torch.equal(got, one[0, :, 0, :, 0].repeat_interleave(3, 0).expand_as(got))
-
-
-@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
 @pytest.mark.parametrize("rows", [3, 40])
 def test_rows_by_place_hold_their_weights_in_float32(dtype, rows):
     """Next to values that some rows do not see and that are not finite, rows go
