@@ -143,7 +143,7 @@ __device__ __forceinline__ float weight2(float s, float base, float scale2, floa
 // the largest stay below 2^16 (the largest of a row is 2^lag in many_kernel,
 // whose references lag): float16 holds 11 bits down to 2^-14 and nothing below
 // 2^-25, and a row's many small weights may be most of its sum.  Raised by 15, a
-// weight of 2^-29 of the largest keeps its bits (by 9, one of 2^-22), and none is off
+// weight of 2^-29 of the largest keeps its bits (by 8, one of 2^-22), and none is off
 // by more than 2^-40 (2^-33) of it.  bfloat16 has float32's range.
 template <class T>
 constexpr float raised(float lag) {
@@ -176,8 +176,8 @@ __device__ __forceinline__ RowTile row_tile(const AttendArgs& a, int64_t tile, i
   return {s, (int)row0, false};
 }
 
-// Powers of two to a unit of many_kernel's references (a power of two itself: whole
-// numbers stay exact), so large that a finite score's never overflows.
+// Powers of two to a unit of many_kernel's references (a power of two itself: they
+// stay exact), so large that a finite score's never overflows.
 constexpr float kBaseUnit = 0x1p64f;
 
 // A sequence, one of its row tiles and one of their runs.

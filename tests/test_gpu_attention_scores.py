@@ -86,6 +86,43 @@ def test_small_weights_add_up(dtype, new, kv, down):
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("rows", [1, 20, 40, 150])
+def test_the_largest_weight_is_exact(dtype, rows):
+    """A row that sees one place (a prompt's first), or one that outweighs the
+    others 2^30 times, gets that place's values bit for bit."""
+    cache, batch, q = _inputs([rows], [rows], 6, 2, 128, 64, dtype, 3, 2.0)
+    vs = S.gather(cache, batch, 0)[1]
+    one = vs[:, 0].to(dtype).repeat_interleave(3, 0)
+    assert torch.equal(_run(cache, batch, q)[0], one)
+    q[..., 0] = 40.0
+    cache["k"][..., 0] = 0.0
+    page = int(batch["page_table"][0, 0])
+    cache["k"][page, :, 0, 0] = 11.0  # 440 / 11.3 above the others' few units: 2^56 and up
+    got = _run(cache, batch, q)
+    assert torch.equal(got, one.expand_as(got))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("value", [700, 715, 718, 1008, 1012, 1013, 1014, 1015])
+def test_rising_scores_beyond_whole_numbers(dtype, value):
+    """Scores of 2^22.9 to 2^24 powers of two that rise by 10 to 20 more behind
+    the first 64 places, whose values are 0: those behind outweigh them at least
+    500 times (float32's steps of 1 there among it)."""
+    cache, batch, q = _inputs([40], [200], 2, 1, 128, 64, dtype, 1)
+    cache["v"].fill_(1)
+    page = int(batch["page_table"][0, 0])
+    cache["v"][page] = 0
+    for up in range(80, 161, 5):
+        cache["k"].fill_(value)
+        cache["k"][..., 127] = up  # times 1 and 0.1275: 10.2 to 20.4 powers of two
+        cache["k"][page, ..., 127] = 0
+        q.fill_(value)
+        q[..., 127] = 1.0
+        got = _run(cache, batch, q).double()
+        assert bool(((got >= 0.99) & (got <= 1)).all()), (up, float(got.min()), float(got.max()))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
 @pytest.mark.parametrize("rows", [3, 40])
 def test_rows_by_place_hold_their_weights_in_float32(dtype, rows):
     """Next to values that some rows do not see and that are not finite, rows go
