@@ -20,7 +20,7 @@
 // large batches and the chain of dependent loads (lengths, pages, K, V, then the
 // join's) small ones.  One token each of 3 requests with up to 131,072 cached, 8 KV
 // heads of 128: 1.35 GB in 243 to 253 us, 5.4 TB/s (a large copy reaches 4.9);
-// of 256 uneven requests with 2 KV heads: 394 MB in 101 us, 3.9 TB/s; of 64: 133
+// of 256 uneven requests with 2 KV heads: 394 MB in 99 us, 4.0 TB/s; of 64: 133
 // MB in 33 us, 4.0 TB/s; one request of 700 tokens: 9.7 us.  Loading a step ahead
 // (32 more tokens in registers) changes nothing: other waves fill the wait.
 #include "serve_device.h"

@@ -16,7 +16,7 @@
 // exponentials, maxima, sums and conversions, which two waves a SIMD overlap in
 // part (3,800 cycles for both); heads of 64 halve the products alone.  Two prompts
 // of 8,192 tokens, 16 heads of 128: 585 to 607 us, 905 to 940 TFLOP/s (a large
-// matrix product reaches 1,407); four of 4,096, heads of 64: 182 us, 755 TFLOP/s.
+// matrix product reaches 1,407); four of 4,096, heads of 64: 179 us, 769 TFLOP/s.
 // Short prompts pay about 6 us a workgroup for its start and end: 29 of 16 to 3,342
 // tokens 152 us, 696 TFLOP/s (159 to 167 us replayed in a graph).  Raising the
 // waves' priority around the products gains nothing (585 to 594 us).
